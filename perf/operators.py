@@ -405,7 +405,6 @@ def run(state):
     s, c = state, state["case"]
     if own and "handle" not in s:
         s["handle"] = _handle(s)
-        s["layers"] = (list(s.get("ks", ())), list(s.get("vs", ())))        # a model holds its layers' keys and values apart
     if c["op"] == "rotate":
         if own:
             s["handle"].rotate(s["positions"], s["q"], s["k"], s["q_out"], s["k_out"])
@@ -421,7 +420,7 @@ def run(state):
         return _plain_attend(s)
     if c["op"] == "store":
         if own:
-            s["handle"].store_layers(0, *s["layers"], s["cu"], s["idx"], s["counts"])
+            s["handle"].store_layers(0, list(s["ks"]), list(s["vs"]), s["cu"], s["idx"], s["counts"])
         else:
             _plain_store(s)
     elif c["op"] == "append":

@@ -101,16 +101,26 @@ class PagedCache:
         """Sequence q goes on from what sequence parents[q] holds, for all q at once; parents[q] outside the batch: it is emptied."""
         self._on(dkv.dkv_pages_fork, self.desc, self.pages, self._ints(parents, self._of_seqs, "parents"), self.ws, stream)
 
-    def _prompt_strides(self, k, v, stride_token, stride_head):
-        """As given, else those of the tensors, [Hkv][tokens][d]."""
+    def _prompt_strides(self, ks, vs, stride_token, stride_head):
+        """As given, else those of the tensors, [Hkv][tokens][d]; the call has one pair of strides for all of them."""
         if stride_token is None or stride_head is None:
             Hkv, d = self._of_row
-            shape, strides = k.shape, k.stride()
-            if len(shape) != 3 or shape[0] != Hkv or shape[2] != d or strides[2] != 1 or v.shape != shape or v.stride() != strides:
-                raise ValueError("k, v: [%d][tokens][%d] with the same strides, or stride_token and stride_head, are required" % (Hkv, d))
+            shape, strides = ks[0].shape, ks[0].stride()
+            alike = len(shape) == 3 and shape[0] == Hkv and shape[2] == d and strides[2] == 1
+            for xs in (ks, vs):
+                for x in xs:
+                    if x.shape != shape or (x.stride() != strides and self._lies_apart(x, strides)):
+                        alike = False
+            if not alike:
+                raise ValueError("k, v: [%d][tokens][%d] with the same tokens and strides, or stride_token and stride_head, are required" % (Hkv, d))
             stride_token = strides[1] if stride_token is None else stride_token
             stride_head = strides[0] if stride_head is None else stride_head
         return stride_token, stride_head
+
+    @staticmethod
+    def _lies_apart(x, strides):
+        """Whether x has other strides, along dimensions of more than one element."""
+        return any(n > 1 and a != b for n, a, b in zip(x.shape, x.stride(), strides))
 
     def _prompt(self, ks, vs, cu_seqlens, idx, of_idx, counts):
         dtype, index, i32 = self.tdtype, self._index, torch.int32
@@ -129,17 +139,18 @@ class PagedCache:
         """The window rows and the retained rows of a layer (idx [n_seqs][Hkv][layer_max], as the selection writes it). k, v: [Hkv][tokens]
         [d], or any order whose strides (in elements) are given."""
         self._prompt((k,), (v,), cu_seqlens, idx, self._of_layer_idx, counts)
-        self._on(dkv.dkv_pages_store, self.desc, layer, self.pages, k, v, *self._prompt_strides(k, v, stride_token, stride_head),
+        self._on(dkv.dkv_pages_store, self.desc, layer, self.pages, k, v, *self._prompt_strides((k,), (v,), stride_token, stride_head),
                  cu_seqlens, idx, counts, stream)
 
     def store_layers(self, layer_begin, ks, vs, cu_seqlens, idx_all, counts, stride_token=None, stride_head=None, stream=None):
-        """The same for consecutive layers in one call (idx_all [L][n_seqs][Hkv][layer_max]; all ks and vs have the same strides)."""
+        """The same for consecutive layers in one call (idx_all [L][n_seqs][Hkv][layer_max]; all ks and vs have the same strides: they are compared
+        unless both strides are given, which then are those of all)."""
         ks, vs = ks if type(ks) is list else list(ks), vs if type(vs) is list else list(vs)
         if not ks or len(ks) != len(vs):
             raise ValueError("as many of v as of k, and one at least: got %d and %d" % (len(vs), len(ks)))
         self._prompt(ks, vs, cu_seqlens, idx_all, self._of_idx, counts)
         self._on(dkv.dkv_pages_store_layers, self.desc, layer_begin, self.pages, ks, vs,
-                 *self._prompt_strides(ks[0], vs[0], stride_token, stride_head), cu_seqlens, idx_all, counts, stream)
+                 *self._prompt_strides(ks, vs, stride_token, stride_head), cu_seqlens, idx_all, counts, stream)
 
     def append(self, layer, k_new, v_new, active=None, stream=None):
         """The last rows of every sequence become the new tokens' [n_seqs][n_new][Hkv][d] (or [n_seqs][Hkv][d]: one token)."""

@@ -154,8 +154,10 @@ class Compressor:
             self._positions = tuple(x.to(device=self.device, dtype=torch.int32).contiguous() for x in (window, token[None]))
         st = d if stride_token is None else stride_token
         sh = cfg.total_tokens * d if stride_head is None else stride_head
+        k = k.as_strided((1, cfg.total_tokens, cfg.Hkv, d), (0, st, sh, 1))
+        rotary._pair(k, None, 1, cfg.total_tokens, "k")       # refused before the queries are written
         rotary.rotate(self._positions[0], q_win.transpose(1, 2), stream=stream)
-        rotary.rotate(self._positions[1], k.as_strided((1, cfg.total_tokens, cfg.Hkv, d), (0, st, sh, 1)), stream=stream)
+        rotary.rotate(self._positions[1], k, stream=stream)
 
     def select_layers(self, layer_begin, n_layers, stream=None):
         dkv.dkv_select_topk_layers(self.desc, layer_begin, n_layers, self.scores, self.cu, self.idx, self.counts,

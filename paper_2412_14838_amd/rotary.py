@@ -43,6 +43,9 @@ class Rotary:
         self.desc = dkv.dkv_rotary(head_dim, rot_dim, int(bool(interleaved)), dtype, factor, self.turns.data_ptr() if rot_dim else None)
 
     def _refuse(self, x, n_seqs, n_tokens, name):
+        if x.requires_grad and torch.is_grad_enabled():
+            raise ValueError("%s requires a gradient, which autograd does not record here: rotate under torch.no_grad(), the gradient with -positions"
+                             % name)
         if x.dtype is not self.tdtype or x.get_device() != self._index:
             raise ValueError("%s: %s on %s is required, got %s on %s" % (name, self.tdtype, self.device, x.dtype, x.device))
         if len(x.shape) != 4 or x.shape[:2] != (n_seqs, n_tokens) or x.shape[3] != self._head:
@@ -56,14 +59,16 @@ class Rotary:
             self._refuse(x, n_seqs, n_tokens, name)
         a, b, heads, d = shape
         seq, token, head, element = strides
-        if a != n_seqs or b != n_tokens or d != self._head or (element != 1 and d > 1) or x.dtype is not self.tdtype or x.get_device() != self._index:
+        if a != n_seqs or b != n_tokens or d != self._head or (element != 1 and d > 1) or x.dtype is not self.tdtype or \
+                x.get_device() != self._index or (x.requires_grad and torch.is_grad_enabled()):
             self._refuse(x, n_seqs, n_tokens, name)
         if out is None or out is x:
             return heads, x, x, (seq, token, head), (seq, token, head)
         if out.shape != shape:
             raise ValueError("%s_out has the shape of %s" % (name, name))
         out_seq, out_token, out_head, element = out.stride()
-        if (element != 1 and d > 1) or out.dtype is not self.tdtype or out.get_device() != self._index:
+        if (element != 1 and d > 1) or out.dtype is not self.tdtype or out.get_device() != self._index or \
+                (out.requires_grad and torch.is_grad_enabled()):
             self._refuse(out, n_seqs, n_tokens, name + "_out")
         return heads, x, out, (seq, token, head), (out_seq, out_token, out_head)
 
@@ -78,7 +83,8 @@ class Rotary:
 
     def rotate(self, positions, q, k=None, q_out=None, k_out=None, stream=None):
         """q (and k) rotated by positions, into q_out and k_out or in place. Negative positions undo positive ones. What is written for
-        the one overlaps neither tensor of the other, and its own input only in place."""
+        the one overlaps neither tensor of the other, and its own input only in place. Nothing is recorded for autograd: tensors that require
+        a gradient are refused unless grad mode is off. The gradient of a rotation is the rotation of the outputs' gradient by -positions."""
         if positions.dim() != 2 or positions.dtype is not torch.int32 or positions.get_device() != self._index or not positions.is_contiguous():
             raise ValueError("positions: contiguous int32 [n_seqs][n_tokens] on %s is required" % self.device)
         n_seqs, n_tokens = positions.shape

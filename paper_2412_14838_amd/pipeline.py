@@ -83,6 +83,13 @@ class Compressor:
             kind = dkv.DKV_SCHEDULE_PYRAMID if schedule == "pyramid" else dkv.DKV_SCHEDULE_FIXED
             self.preset = torch.tensor(dkv.dkv_layer_budgets(self.desc, kind, beta), dtype=torch.int32, device=device)
 
+    def __getattr__(self, name):
+        # reached for what is not there only
+        if name in ("kb", "vb"):
+            raise AttributeError("Compressor.%s: %s" % (name, "no padded blocks, keep_cache is False" if self.__dict__.get("pages") is None else
+                                                        "the rows are in the PagedCache that `pages` names, decode with its calls"))
+        raise AttributeError("%r object has no attribute %r" % (type(self).__name__, name))
+
     @property
     def budgets(self):
         return self.budgets_all[self._last_update]

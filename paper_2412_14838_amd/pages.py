@@ -20,8 +20,12 @@ _DTYPES = {dkv.DKV_BF16: torch.bfloat16, dkv.DKV_F32: torch.float32}
 _current_device = getattr(torch._C, "_cuda_getDevice", None)        # what torch.cuda.current_device() asks, without its start-up
 
 
+NEW_ROWS = 1024                     # room for new tokens behind a prompt's rows where max_rows is not given
+
+
 class PagedCache:
-    """desc: the dkv_desc of the sequences that share the pool. max_rows: rows that one (sequence, layer) can hold (rounded up to pages).
+    """desc: the dkv_desc of the sequences that share the pool. max_rows: rows that one (sequence, layer) can hold (rounded up to pages);
+    by default all that a prompt can leave, window + layer_max, and NEW_ROWS, or as many as a table that is handed over has entries for.
     The tensors (k, v as torch.float8_e4m3fn, k_scale, v_scale, table, rows, refs, missing; shapes as in include/dkv.h) are allocated
     and cleared, unless the caller hands over its own."""
 
@@ -30,9 +34,13 @@ class PagedCache:
         L, Hkv, d, n_seqs = desc.n_layers, desc.n_kv_heads, desc.head_dim, desc.n_seqs
         if page_rows not in (16, 32, 64, 128) or n_pages < 1:
             raise ValueError("page_rows is 16, 32, 64 or 128 and n_pages at least 1: got %r, %r" % (page_rows, n_pages))
-        max_rows = desc.window + desc.layer_max if max_rows is None else max_rows
-        table_len = max(-(-max_rows // page_rows), 1)
+        by_default, table, prompt = max_rows is None, tensors.get("table"), desc.window + desc.layer_max
+        table_len = max(-(-(prompt + NEW_ROWS if by_default else max_rows) // page_rows), 1)
+        if by_default and table is not None and table.dim() == 3:
+            table_len = max(table.shape[2], 1)
         self.max_rows = table_len * page_rows
+        # attention's hint where the caller has none: that the tables have room for new tokens does not make the prompt's rows more
+        self._expected = -(-prompt // page_rows) * page_rows if by_default and table is None else 0
         shapes = {"k": ((n_pages, Hkv, page_rows, d), torch.float8_e4m3fn), "v": ((n_pages, Hkv, d, page_rows), torch.float8_e4m3fn),
                   "k_scale": ((n_pages, Hkv), torch.float32), "v_scale": ((n_pages, Hkv), torch.float32),
                   "table": ((n_seqs, L, table_len), torch.int32), "rows": ((n_seqs, L), torch.int32),
@@ -170,12 +178,14 @@ class PagedCache:
                  self._ints(active, self._of_seqs, "active"), stream)
 
     def attention(self, layer, q_new, out, lse_out=None, expected_rows=0, stream=None):
-        """Attention of one new token per sequence (q_new [n_seqs][Hq][d]) over layer `layer`; out fp32 like q_new, lse_out [n_seqs][Hq]."""
+        """Attention of one new token per sequence (q_new [n_seqs][Hq][d]) over layer `layer`; out fp32 like q_new, lse_out [n_seqs][Hq].
+        expected_rows: how many rows there are, about; it decides the time, and the split over workgroups that pays for long rows costs
+        short ones a launch. 0: as many as max_rows, or, where that is the default, as a prompt leaves at most."""
         self._whole(q_new, self._of_q, self.tdtype, "q_new")
         self._whole(out, self._of_q, torch.float32, "out")
         if lse_out is not None:
             self._whole(lse_out, self._of_lse, torch.float32, "lse_out")
-        self._on(dkv.dkv_pages_attention, self.desc, layer, self.pages, expected_rows, q_new, out, lse_out, self.ws, stream)
+        self._on(dkv.dkv_pages_attention, self.desc, layer, self.pages, expected_rows or self._expected, q_new, out, lse_out, self.ws, stream)
 
     def attention_layers(self, layer_begin, n_layers, q_new_all, out_all, lse_all=None, expected_rows=0, stream=None):
         """The same for n_layers consecutive layers in one call: q_new_all, out_all [n_layers][n_seqs][Hq][d]."""
@@ -183,5 +193,5 @@ class PagedCache:
         self._whole(out_all, (n_layers,) + self._of_q, torch.float32, "out_all")
         if lse_all is not None:
             self._whole(lse_all, (n_layers,) + self._of_lse, torch.float32, "lse_all")
-        self._on(dkv.dkv_pages_attention_layers, self.desc, layer_begin, n_layers, self.pages, expected_rows, q_new_all, out_all, lse_all,
-                 self.ws, stream)
+        self._on(dkv.dkv_pages_attention_layers, self.desc, layer_begin, n_layers, self.pages, expected_rows or self._expected, q_new_all, out_all,
+                 lse_all, self.ws, stream)

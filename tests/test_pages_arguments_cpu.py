@@ -55,3 +55,32 @@ def test_layers_of_one_call_are_laid_out_alike(seen):
     # given strides say how all of them lie, whatever their shapes
     cache.store_layers(0, [_bf(60 * 2 * 128)] * 2, [_bf(60, 2, 128)] * 2, *rest, stride_token=256, stride_head=128)
     assert seen[-1][1][5:7] == (256, 128)
+
+
+def test_room_for_new_tokens_by_default(seen):
+    """A layer that holds all that a prompt can leave still takes new rows; attention goes on expecting what a prompt leaves."""
+    d = _desc()                                           # 16 + 64 rows of a prompt
+    cache = PagedCache(d, n_pages=10, page_rows=16, device="cpu")
+    assert cache.max_rows >= 80 + 1024 and cache.table.shape == (3, 4, cache.max_rows // 16)
+    q, out = _bf(2, 3, 4, 128), torch.zeros(2, 3, 4, 128)
+
+    def hints(cache):
+        seen.clear()
+        for rows in (0, 33):
+            cache.attention(0, q[0], out[0], expected_rows=rows)
+            cache.attention_layers(0, 2, q, out, expected_rows=rows)
+        return [a[4 if name == "attention_layers" else 3] for name, a in seen]
+
+    assert hints(cache) == [80, 80, 33, 33]
+    assert hints(PagedCache(d, n_pages=10, page_rows=64, device="cpu")) == [128, 128, 33, 33]        # what two pages hold
+    named = PagedCache(d, n_pages=10, page_rows=16, max_rows=80, device="cpu")
+    assert named.max_rows == 80 and hints(named) == [0, 0, 33, 33]
+    # tables of the caller's own say themselves how long they are
+    tensors = {name: getattr(named, name) for name in ("k", "v", "k_scale", "v_scale", "table", "rows", "refs", "missing")}
+    for length in (5, 7):
+        tensors["table"] = _i32(3, 4, length)
+        own = PagedCache(d, n_pages=10, page_rows=16, device="cpu", **tensors)
+        assert own.max_rows == 16 * length and own.pages.table_len == length and hints(own) == [0, 0, 33, 33]
+    for bad in (_i32(3, 4, 0), _i32(3, 4), _i32(4, 3, 5)):
+        with pytest.raises(ValueError):
+            PagedCache(d, n_pages=10, page_rows=16, device="cpu", **dict(tensors, table=bad))

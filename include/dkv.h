@@ -463,8 +463,9 @@ int dkv_select_recent(const dkv_desc* desc, int32_t layer, int32_t n_sink, const
  *            table[q][l][r / page_rows]. Entries past the pages in use are -1 and are not read.
  *   rows     int32 [n_seqs][L]: rows that (q, l) holds; 0 .. table_len * page_rows.
  *   refs     int32 [n_pages]: table entries that name the page; 0: the page is free. 16-byte aligned.
- *   missing  int32 [1]: 0, or the pages that a dkv_pages_resize call lacked. From then on no call grows a sequence or writes rows, until
- *            the caller has read it, made room (sequences still shrink and end) and set it back to 0.
+ *   missing  int32 [1]: 0, or the pages that a dkv_pages_resize call lacked. From then on no page is granted and no row written, until
+ *            the caller has read it, made room and set it back to 0. Sequences still shrink and end, and dkv_pages_fork still does
+ *            all that it does (it needs no page).
  * A scale is the smallest power of two with |x| <= 448 * scale for all finite elements of its block (a floating-point code
  * keeps its relative precision under any such scale, and a block that is scaled anew loses nothing but the smallest codes);
  * codes are rounded to nearest even, infinite elements become the largest code, NaN stays NaN.
@@ -501,7 +502,8 @@ int dkv_pages_clear(const dkv_desc* desc, const dkv_pages* pages, void* stream);
  * First, where target < rows, the pages behind the last row are given back (a page is free when no table names it) and rows is
  * set. Then, where target > rows, pages are granted: the free pages with the lowest numbers, to the sequences in order and within
  * a sequence to the layers in order. A last page that is not full and that other tables name too is replaced by a copy of it,
- * so that the new rows are the sequence's own; where several of its owners grow in the same call each gets a copy. Growth is all or
+ * so that the new rows are the sequence's own; where several of its owners grow in the same call each gets a copy (k owners take k free
+ * pages, and the page that nobody names any more is free afterwards, not yet for this call). Growth is all or
  * nothing: if the pool has too few free pages, or a target does not fit the table, no (q, l) of the call grows and *missing becomes
  * the number of pages that lack (in the pool, and past the tables' ends); if *missing was not 0 before, nothing grows either and it
  * stays. The new rows hold whatever their pages held. Two kernels (the tables by one workgroup, then the copies; one kernel where nothing can grow: base = pages->rows,
@@ -539,7 +541,7 @@ int dkv_pages_store_layers(const dkv_desc* desc, int32_t layer_begin, int32_t n_
  * values (dkv_pages_resize with extra = n_new comes first). A page that holds earlier rows keeps its scale unless the new rows
  * need a larger one; then the earlier rows' codes are rounded once more, to the new scale. Rows before the first are left out.
  * Nothing is written for sequences with active[q] == 0 (NULL: all are active), while *missing is not 0, and never to a page that
- * several tables name.
+ * several tables name (a fork comes before the growth, which then copies such a page; forked in between, the rows are left out).
  * k_new, v_new   element (sequence q, new token t, head h, j) at x[q * stride_seq + t * stride_token + h * stride_head + j]
  *                (elements, all strides the same for both), rows 16-byte aligned.
  * n_new          1 .. table_len * page_rows. One kernel.

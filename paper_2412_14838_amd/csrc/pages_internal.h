@@ -74,7 +74,8 @@ __device__ inline int held_rows(const PageArgs& a, int pair) {
 //   16    6.6 / 9.6  10.4 / 12.3 13.3 / 17.2 16.1 / 19.1 27.4 / 28.7  52.0 / 48.0
 //   32   7.3 / 12.1  14.1 / 19.0 19.1 / 24.2 23.6 / 28.5 43.3 / 47.5  99.0 / 104
 //   64  16.9 / 19.9  26.5 / 29.6 35.3 / 39.1 44.7 / 49.0  99.8 / 105   192 / 199
-// With 16 sequences of 4 KV heads and 8192 to 32768 rows the longest decides: 101 / 65.
+// With 16 sequences of 4 KV heads and 8192 to 32768 rows the longest decides: 101 / 65. For that the rule takes pieces for 65 to 512 items of
+// 4096 rows and more although equal rows lose by it: 128 items 5 % at 4096 rows, 256 items 10 and 5 % at 4096 and 8192, 512 items 5 and 4 %.
 inline int pages_groups(int Hkv, int pairs, int rows) {
   const int cus = device_cus(), resident = 2 * (cus < 1024 ? cus : 1024);
   const int64_t items = (int64_t)Hkv * pairs;

@@ -6,9 +6,10 @@ there, one byte an element. Every call is one dkv_pages_* call; the row counts s
     cache = PagedCache(comp.desc, n_pages=4096, max_rows=8192)
     cache.resize(comp.counts, cu_seqlens=comp.cu)                       # room for the window rows and the retained rows
     cache.store_layers(0, ks, vs, comp.cu, comp.idx, comp.counts)       # (or Compressor(cfg, pages=cache), which does both)
-    per token:  cache.resize(cache.rows, 1)
-                per layer:  cache.append(l, k_new, v_new);  cache.attention(l, q_new, out)
-    beams:      cache.fork(parents)
+    per token:  cache.fork(parents)                                     # beams: before the growth, which copies what they share
+                cache.resize(cache.rows, 1)
+                per layer:  cache.append(l, k_new, v_new);  cache.attention(l, q_new, out, expected_rows=about_as_many)
+    now and then:  cache.missing                                        # not 0: the pool was too small, nothing was written since
 """
 from __future__ import annotations
 
@@ -106,7 +107,8 @@ class PagedCache:
                  self._ints(active, self._of_seqs, "active"), self.ws, stream)
 
     def fork(self, parents, stream=None):
-        """Sequence q goes on from what sequence parents[q] holds, for all q at once; parents[q] outside the batch: it is emptied."""
+        """Sequence q goes on from what sequence parents[q] holds, for all q at once; parents[q] outside the batch: it is emptied. Before
+        the resize that makes room for new rows: that copies a last page that is shared, and append writes to no page that is."""
         self._on(dkv.dkv_pages_fork, self.desc, self.pages, self._ints(parents, self._of_seqs, "parents"), self.ws, stream)
 
     def _prompt_strides(self, ks, vs, stride_token, stride_head):
@@ -161,7 +163,8 @@ class PagedCache:
                  *self._prompt_strides(ks, vs, stride_token, stride_head), cu_seqlens, idx_all, counts, stream)
 
     def append(self, layer, k_new, v_new, active=None, stream=None):
-        """The last rows of every sequence become the new tokens' [n_seqs][n_new][Hkv][d] (or [n_seqs][Hkv][d]: one token)."""
+        """The last rows of every sequence become the new tokens' [n_seqs][n_new][Hkv][d] (or [n_seqs][Hkv][d]: one token); k_new and v_new
+        have the same strides. Rows in a page that several sequences share, and all rows while cache.missing is not 0, are left out."""
         shape, strides = k_new.shape, k_new.stride()
         if v_new.shape != shape or v_new.stride() != strides or strides[-1] != 1:
             raise ValueError("k_new and v_new have the same shape and strides, with the elements of a row side by side")
